@@ -161,10 +161,11 @@ __global__ __launch_bounds__(BM * BN / WN) void k_conv_f32(const ConvF32Params p
     auto load = [&](int t, int i) {
         const int s = t % STAGES;
         if (i < AL)
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+            // (a load that takes its LDS address from M0 needs one wait state behind the write of M0)
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                          :: "v"(oa[i < AL ? i : 0]), "s"(ab), "s"(lds_a0 + s * BM * 192 + NTH * 16 * i) : "memory", "m0");
         else
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                          :: "v"(ob[i < AL ? 0 : i - AL]), "s"(bb), "s"(lds_b0 + s * BN * 192 + NTH * 16 * (i - AL))
                          : "memory", "m0");
     };

@@ -297,13 +297,14 @@ __global__ __launch_bounds__(AT) void k_attn_i32r(const AttnParams p) {
         for (int I = (int)wave_u; I < nk; I += 4) {
             const int q = I * 64 + lane, row = q / CK, pos = q % CK;
             const unsigned off = (unsigned)(row * D + ((pos ^ swz_k<D>(row)) * 16));
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+            // (a load that takes its LDS address from M0 needs one wait state behind the write of M0)
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                          :: "v"(off), "s"(k8), "s"(lds_k + I * 1024) : "memory", "m0");
         }
         for (int I = (int)wave_u; I < nv; I += 4) {
             const int q = I * 64 + lane, row = q / CV, pos = q % CV;
             const unsigned off = (unsigned)(row * p.Lp + ((pos ^ swz_v(row, vmask)) * 16));
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                          :: "v"(off), "s"(v8), "s"(lds_v + I * 1024) : "memory", "m0");
         }
     }
@@ -470,11 +471,11 @@ __global__ __launch_bounds__(512) void k_attn_i32s(const AttnParams p) {
             const unsigned dst = lds + (unsigned)(e * BLK + part * 1024);
             if (part < NTO) {
                 const char* kb = K8 + bg * 32 * D;
-                asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                              :: "v"(koff + part * 32), "s"(kb), "s"(dst) : "memory", "m0");
             } else {
                 const char* vb = V8 + bg * D * 32;
-                asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                              :: "v"(voff + (part - NTO) * 1024), "s"(vb), "s"(dst) : "memory", "m0");
             }
         }
@@ -489,7 +490,7 @@ __global__ __launch_bounds__(512) void k_attn_i32s(const AttnParams p) {
         const unsigned dst = (unsigned)(uintptr_t)&qs[wave][0];
 #pragma unroll
         for (int t = 0; t < NTO; ++t)
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                          :: "v"(qoff + 32 * t), "s"(qb), "s"(dst + t * 1024) : "memory", "m0");
     }
     for (int pr = 0; pr < R - 1 && pr < npair; ++pr) issue(pr);

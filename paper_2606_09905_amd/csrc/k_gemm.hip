@@ -1096,11 +1096,12 @@ __global__ __launch_bounds__(64 * WAVES) void k_gemm_i8nt(const GemmParams p) {
         for (int k = 0; k < LAB; ++k) {
             const unsigned blk = wl_u + GW * k;
             const char* base = (int)blk * 64 < CH_A ? ab : bb;
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+            // (a load that takes its LDS address from M0 needs one wait state behind the write of M0)
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                          :: "v"(ol[k]), "s"(base), "s"(ls + blk * 1024) : "memory", "m0");
         }
         if constexpr (OFFS)
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1"
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
                          :: "v"(cs_off), "s"(nhwc ? csg + s_off : csg + (int64_t)t * p.N), "s"(lds_cs0 + s * GTH * 4)
                          : "memory", "m0");
     };
@@ -1139,7 +1140,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_gemm_i8nt(const GemmParams p) {
         for (int I = (int)wave_u; I < BM / 64; I += NTH / 64) {
             const unsigned off = (unsigned)min(m0 + I * 64 + lane, p.M - 1) * 4u;
             const unsigned lds = (unsigned)(uintptr_t)&rs_l[I * 64];
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1"
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
                          :: "v"(off), "s"(rsg), "s"(lds) : "memory", "m0");
         }
     }

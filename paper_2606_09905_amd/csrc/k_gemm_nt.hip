@@ -386,11 +386,12 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_nt(const GemmParams p) {
         const unsigned la = lds_a0 + s * STAGE_A, lb = lds_b0 + s * STAGE_B;
 #pragma unroll
         for (int i = 0; i < AL; ++i)
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+            // (a load that takes its LDS address from M0 needs one wait state behind the write of M0)
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                          :: "v"(oa[i]), "s"(ab), "s"(la + NTH * 16 * i) : "memory", "m0");
 #pragma unroll
         for (int i = 0; i < BL; ++i)
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                          :: "v"(ob[i]), "s"(bb), "s"(lb + NTH * 16 * i) : "memory", "m0");
     };
 

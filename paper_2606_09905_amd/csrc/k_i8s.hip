@@ -243,7 +243,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_i8s(const GemmI8sParams p
                 const int8_t* at = src[i] + (int64_t)t * BK;
                 // pieces past K (the last tile's) come from zeros
                 if (t >= whole && t * BK + sk[i] >= p.K) at = (const int8_t*)&g_zero16;
-                asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off"
+                // (a load that takes its LDS address from M0 needs one wait state behind the write of M0)
+                asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                              :: "v"(at), "s"(base + i * NTH * 16) : "memory", "m0");
             }
         } else {
