@@ -220,7 +220,9 @@ def run(s):
         if own:
             return qx.linear_i8(s["x"], s["w"], s["scale_w"], bias=s["bias_t"])
         x = s["x"].float()
-        sa = x.abs().amax(1) / 127
+        # (a GPU tensor over a plain number is multiplied by its rounded reciprocal: a step off in
+        # one scale of twenty, and with it values next to a half on the other side)
+        sa = (x.abs().amax(1).double() / 127).float()
         a = torch.round(x / sa[:, None]).clamp(-127, 127)
         return _plain_product(a, sa, s["w"], s["scale_w"], s["bias_t"], T)
     if op == "product":
@@ -278,10 +280,12 @@ def exact(case, seed):
     op = case["op"]
     if op in ("linear", "product"):
         if op == "linear":
-            # the scale and the 8-bit values are defined by single-precision arithmetic
-            x = s["x"].to(torch.float32)
-            sa = torch.max(torch.abs(x), dim=1).values / 127.0
-            a = torch.clamp(torch.round(torch.div(x, sa.unsqueeze(1))), -127, 127)
+            # the scale and the 8-bit values are defined by single-precision arithmetic, each
+            # quotient rounded once: from 64 bits, which hold it far enough for that
+            x = s["x"].to(torch.float64)
+            sa = torch.div(torch.max(torch.abs(x), dim=1).values, 127.0).to(torch.float32)
+            a = torch.div(x, sa.to(torch.float64).unsqueeze(1)).to(torch.float32)
+            a = torch.clamp(torch.round(a), -127, 127)
         else:
             a, sa = s["a"], s["scale_a"]
         y = torch.mm(a.double(), s["w"].double().t().contiguous())      # whole numbers below 2^53
