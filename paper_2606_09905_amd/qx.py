@@ -424,16 +424,17 @@ def _ok(t, dev, dtype, shape):
     return t is None or (t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous())
 
 
-def _new(like, shape, dtype, stream):
+def _new(like, shape, dtype, stream, zeros=False):
     """A new tensor on the stream that is going to use it: one of the current
     stream's could be taken up again while another stream still works on it."""
+    make = like.new_zeros if zeros else like.new_empty
     if stream is None:
-        return like.new_empty(shape, dtype=dtype)
+        return make(shape, dtype=dtype)
     cuda = _torch_module.cuda
     if not hasattr(stream, "cuda_stream"):
         stream = cuda.ExternalStream(int(stream)) if int(stream) else cuda.default_stream()
     with cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
+        return make(shape, dtype=dtype)
 
 
 def _workspace(query, dt, sizes, like, workspace, stream):
@@ -552,9 +553,9 @@ def lin_attn(q, k, v, log_decay, scale: float = 1.0, state=None, lens=None, out=
         S_i = exp(log_decay[h]) S_{i-1} + k_i^T v_i,   o_i = scale q_i S_i
     q, k [B, H, L, dk], v [B, H, L, dv] of one floating type, any strides with
     a contiguous last dimension; log_decay [H], state [B, H, dk, dv] float32
-    (None: zeros); lens [B] int32 (None: L), rows behind a sequence's end are
-    left as they were.  Returns (out, state after the last token);
-    out_state may be `state` itself."""
+    (None: zeros); lens [B] int32 (None: L), rows of `out` behind a sequence's
+    end are left as they were, zeros where the call makes it.  Returns (out,
+    state after the last token); out_state may be `state` itself."""
     T = q.dtype
     dt = _float_type(T, "q")
     shape = q.shape
@@ -565,7 +566,7 @@ def lin_attn(q, k, v, log_decay, scale: float = 1.0, state=None, lens=None, out=
     dev = q.get_device()
     vs, ss = (B, H, L, dv), (B, H, dk, dv)
     if out is None:
-        out = _new(q, vs, T, stream)
+        out = _new(q, vs, T, stream, lens is not None)
     if out_state is None:
         out_state = _new(q, ss, _t_f32, stream)
     if (dev < 0 or dev != _get_device() or k.dtype is not T or v.dtype is not T or out.dtype is not T or
@@ -618,7 +619,8 @@ def lin_attn_backward(q, k, v, d_out, log_decay, scale: float = 1.0, state=None,
                       out_state=None, workspace=None, stream=None):
     """Gradients (dq, dk, dv, dstate) of lin_attn from d_out [B, H, L, dv] and
     d_state [B, H, dk, dv] (None: zeros), the gradients of its two results.
-    `out`: three tensors for dq, dk, dv; rows behind a sequence's end are left as they were."""
+    `out`: three tensors for dq, dk, dv, whose rows behind a sequence's end are
+    left as they were; zeros where the call makes them."""
     T = q.dtype
     dt = _float_type(T, "q")
     shape = q.shape
@@ -629,7 +631,7 @@ def lin_attn_backward(q, k, v, d_out, log_decay, scale: float = 1.0, state=None,
     dev = q.get_device()
     vs, ss = (B, H, L, dv), (B, H, dk, dv)
     if out is None:
-        out = [_new(q, t, T, stream) for t in (shape, shape, vs)]
+        out = [_new(q, t, T, stream, lens is not None) for t in (shape, shape, vs)]
     gq, gk, gv = out
     if out_state is None:
         out_state = _new(q, ss, _t_f32, stream)
