@@ -258,7 +258,7 @@ qx_status quantize_rows_i8(qx_float_type dt, const void* x, int8_t* q, float* sc
  *   Y[m][n] = scale_a[m] scale_w[n] sum_k A[m][k] W[n][k] + bias[n]
  * A [M][K] int8, W [N][K] int8 (a linear layer's weights: an output channel a
  * row), Y [M][N] of type dt, bias [N] or NULL.  Any int8 values; the sum is
- * exact.  M, N in [0, 2^23], K in [0, 131071], M N <= 2^37. */
+ * exact, and the scaled sum is finite in fp32 wherever its value is.  M, N in [0, 2^23], K in [0, 131071], M N <= 2^37. */
 qx_status qgemm_i8_scaled(qx_float_type dt, const int8_t* A, const int8_t* W, const float* scale_a,
                           const float* scale_w, const float* bias, void* Y, int64_t M, int64_t N, int64_t K,
                           void* stream);

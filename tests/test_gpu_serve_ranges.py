@@ -72,3 +72,50 @@ def test_rows_behind_the_end_of_a_callers_gradients_stay(dtype, L, dk, dv):
         for b in range(B):
             assert (t[b, :, n[b]:] == 7).all()
             assert ref.norm_error(t[b, :, :n[b]], w[b, :, :n[b]]) <= ref.norm_tolerance(dtype)
+
+
+# ---------------------------------------------------------------------------
+# scales
+# ---------------------------------------------------------------------------
+# one launch, rows kernels, and tiles of aligned and of unaligned rows, in every tile size
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,N,K", [(2, 40, 300), (12, 70, 2048), (20, 2100, 160), (70, 130, 128), (70, 130, 77),
+                                   (600, 9000, 256), (4096, 4200, 64), (4096, 4200, 65)])
+def test_large_rows_and_small_weights(dtype, M, N, K):
+    """A product with one scale may pass the range of float32 where the result does not."""
+    g = gen(M + K)
+    x = normal(g, M, K, dtype=dtype)
+    w = torch.randint(-128, 128, (N, K), generator=g, dtype=torch.int32).to(torch.int8).cuda()
+    sw = torch.rand(N, generator=g).cuda() * 1e-3
+    bias = normal(g, N)
+    plain = qx.linear_i8(x, w, sw, bias=bias)
+    rows = torch.arange(0, M, 3, device="cuda")
+    big = x.clone()
+    big[rows] = (x[rows].float() * 3e37 / x[rows].float().abs().amax(1, keepdim=True)).to(dtype)
+    if M > 10:
+        big[4, 1] = float("nan")
+    y = qx.linear_i8(big, w, sw, bias=bias)
+    a, sa = qx.quantize_rows_i8(big)
+    assert torch.equal(y.nan_to_num(), qx.qgemm_i8_scaled(a, w, sa, sw, bias=bias, dtype=dtype).nan_to_num())
+    other = torch.ones(M, dtype=torch.bool, device="cuda")
+    other[rows] = False
+    if M > 10:
+        assert torch.isnan(y[4]).all()
+        other[4] = False
+    assert torch.equal(y[other], plain[other])
+    want, tol = ref.product(ref.quantize(big[rows])[0], w, ref.quantize(big[rows])[1], sw, bias)
+    assert float(want.abs().max()) < 3e38 and float((want / sw.cpu()).abs().max()) > 3.5e38     # what this is about
+    if dtype != F32:
+        tol = tol + ref.half_ulp(dtype) * (want.abs() + tol)
+    assert ((y[rows].cpu().double() - want).abs() <= tol).all()
+
+
+def test_small_rows_and_large_weights():
+    # and the other way round, with a sum of nothing: 0 times the product of both scales would be NaN
+    a = torch.tensor([[1, -1], [1, 1]], dtype=torch.int8, device="cuda")
+    w = torch.tensor([[1, 1], [127, -128]], dtype=torch.int8, device="cuda")
+    sa, sw = torch.tensor([1e30, 1e-30], device="cuda"), torch.tensor([1e30, 1e10], device="cuda")
+    y = qx.qgemm_i8_scaled(a, w, sa, sw, dtype=F32).cpu()
+    assert y[0, 0] == 0 and y[0, 1] == float("inf")
+    want, tol = ref.product(a, w, sa, sw)
+    assert ((y[1].double() - want[1]).abs() <= tol[1]).all()
