@@ -280,7 +280,8 @@ qx_status linear_i8(qx_float_type dt, const void* x, const int8_t* W, const floa
  *
  * Q, K [B][H][L][dk], V, O [B][H][L][dv] of type dt; states [B][H][dk][dv]
  * float32, dense; log_decay [H], meant to be <= 0, -inf for no
- * memory (larger values grow, and overflow as they would).  strides: NULL
+ * memory (larger values grow, and overflow as they would); a decay close to one
+ * keeps its rate to 2^-23 of it however often it is applied.  strides: NULL
  * for dense arrays, else the (batch, head, row) strides of Q, K, V, O in
  * elements, 12 values, each in [0, 2^40]; the last dimension is contiguous;
  * inputs may have strides of 0, elements of O may not share addresses.

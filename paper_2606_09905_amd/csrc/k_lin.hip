@@ -118,6 +118,50 @@ __device__ __forceinline__ float decay_pow(float g, int n) {
     return n == 0 ? 1.f : __builtin_amdgcn_exp2f((float)((double)g * 1.4426950408889634 * n));
 }
 
+// The rounding of a factor close to one is a change of the decay, the same one
+// each time it is applied: at g = -1e-6, token by token, 1.3% of it.
+//
+// One token's: s exp(g) + more, as s + (s (exp(g) - 1) + more) where exp(g) is
+// more than a half.
+struct Decay {
+    float f;      // exp(g n) - 1, or exp(g n)
+    bool near;    // (the same for all threads of a head)
+    __device__ __forceinline__ float of(float s, float more) const {
+        const float t = __builtin_fmaf(s, f, more);
+        return near ? s + t : t;
+    }
+};
+__device__ __forceinline__ Decay decay_of(float g, int n) {
+    const double x = (double)g * n;
+    const bool near = x > -0.69;
+    const float less = expm1f((float)x), whole = decay_pow(g, n);   // (both: a branch would hold back the loads behind it)
+    return {near ? less : whole, near};
+}
+// The factors exp(g n) for one step of n tokens after the other: of the two
+// floats around it now one, now the other, so that the product of any number
+// of them is a rounding off.  (The two terms above for each element of the
+// state cost 5% to 37% of the time of all chunks; a wave's these are two scalar adds.)
+struct Factors {
+    uint32_t lo, part, at;   // the smaller float; how far, in 2^-32, exp(g n) lies past it; what has gathered
+    __device__ __forceinline__ float next() {
+        const uint32_t was = at;
+        at += part;
+        return __uint_as_float(lo + (at < was ? 1u : 0u));
+    }
+};
+__device__ __forceinline__ Factors factors_of(float g, int n) {
+    const double x = (double)g * n;
+    const bool near = fabs(x) < 0.69;
+    const float e = near ? expm1f((float)x) : 0.f;
+    const float k = e * (e < 0.f ? 0x1p24f : 0x1p23f), f = floorf(k);   // in places of the floats below or above one
+    const uint32_t lo = __float_as_uint(near ? 1.f + f * (e < 0.f ? 0x1p-24f : 0x1p-23f) : decay_pow(g, n));
+    const uint32_t part = (uint32_t)fminf((k - f) * 0x1p32f, 4294967040.f);
+    return {lo, part, 0x80000000u};
+}
+__device__ __forceinline__ Factors for_wave(const Factors& f) {
+    return {(uint32_t)__builtin_amdgcn_readfirstlane((int)f.lo), (uint32_t)__builtin_amdgcn_readfirstlane((int)f.part), 0x80000000u};
+}
+
 // Eight elements: all of them, or the first n with zeros behind them; raw
 // 16-bit words or floats.
 template <class E>
@@ -301,6 +345,7 @@ __global__ __launch_bounds__(64 * W, DX <= 128 ? 2 : 1) void k_lin(const LinPara
     __shared__ __align__(16) uint16_t Ys[NB][T][CH][DXP];
     __shared__ __align__(16) uint16_t Zs[NB][T][CH][ZP];
     __shared__ float pw[CH + 1], pu[2 * CH];               // powers of the decay; the update's weights
+    __shared__ Factors fs;                                 // of a whole chunk
     __shared__ int odd[2];                                 // the last chunk (of even and odd ones) whose z is not finite
 
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
@@ -426,6 +471,7 @@ __global__ __launch_bounds__(64 * W, DX <= 128 ? 2 : 1) void k_lin(const LinPara
     // j + 32 - n here, zeros behind the end
     if (tid < 2 * CH) pu[tid] = tid < CH ? decay_pow(g, CH - 1 - tid + p.rev) * p.u_mul : 0.f;
     if (tid < 2) odd[tid] = -1;
+    if (tid == NTH - 1) fs = factors_of(g, CH);            // (a wave that has none of the above)
     __syncthreads();
     // the state: element (a, c0 + l32) of register r of tile a / 32, a = 8 (r / 4) + 4 hh + r % 4
     f16x S[AT];
@@ -471,8 +517,9 @@ __global__ __launch_bounds__(64 * W, DX <= 128 ? 2 : 1) void k_lin(const LinPara
         // few and small states: each segment adds up those before it, which
         // saves the scan
         if (!STATE && p.prefix && live) {
-            const float lam = decay_pow(g, p.seg_len);
+            Factors of_segments = for_wave(factors_of(g, p.seg_len));
             for (int t = 0; t < seg; ++t) {
+                const float lam = of_segments.next();
                 const float* u = p.U + frag - (int64_t)(seg - t) * W * (AT * 4 * 256);
 #pragma unroll
                 for (int k = 0; k < AT * 4; ++k) {
@@ -497,6 +544,7 @@ __global__ __launch_bounds__(64 * W, DX <= 128 ? 2 : 1) void k_lin(const LinPara
     // this lane's row of the output: token l32, or from the end
     char* orow = (char*)p.O + (b * p.so[0] + h * p.so[1] + (first + dir * l32) * p.so[2]) * ES;
     const int64_t mo = dir * CH * p.so[2] * ES;
+    Factors of_chunks = for_wave(fs);
 
     for (int tc = t0, par = 0; tc < t1; tc += CH, par ^= 1) {
         const int buf = NB == 2 ? par : 0;
@@ -531,7 +579,7 @@ __global__ __launch_bounds__(64 * W, DX <= 128 ? 2 : 1) void k_lin(const LinPara
                             yt[i & 1][k][n] = join(read_tr(&Ys[buf][n][j][c + 32 * k]), read_tr(&Ys[buf][n][j + 8][c + 32 * k]));
                     }
             };
-            const float wc = pw[cnt];
+            const float wc = cnt == CH ? of_chunks.next() : pw[cnt];
             f16x P{}, O{};
             if constexpr (!STATE) {
                 b8 x[2][T], y[2][T];
@@ -711,7 +759,7 @@ __global__ __launch_bounds__(256) void k_lin_scan(const LinParams p) {
     const int c = (zt * waves + wave) * 32 + (lane & 31), a0 = 32 * (grp >> 2) + 8 * (grp & 3) + 4 * (lane >> 5);
     if (c >= p.dz) return;
     const int len = p.lens ? min(max(p.lens[b], 0), p.L) : p.L;
-    const float lam = decay_pow(p.g[h], p.seg_len);
+    const Decay lam = decay_of(p.g[h], p.seg_len);
     const int ra = p.s_t ? 1 : p.dz, rc = p.s_t ? p.dx : 1;
     f4 cur;
 #pragma unroll
@@ -734,7 +782,7 @@ __global__ __launch_bounds__(256) void k_lin_scan(const LinParams p) {
             if (s0 + k < n) {
                 *(f4*)(u + (s0 + k) * per * 4) = cur;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) cur[e] = cur[e] * lam + v[k][e];
+                for (int e = 0; e < 4; ++e) cur[e] = lam.of(cur[e], v[k][e]);
             }
     }
 }
@@ -767,7 +815,7 @@ __global__ __launch_bounds__(256) void k_lin_step(const LinStepParams p) {
     float* S = p.S + bh * p.dk * p.dv;
     // full vectors where rows keep their 16 bytes, else element by element
     const bool vec = p.dv % 4 == 0 && ((uintptr_t)p.S & 15) == 0;
-    const float lam = decay_pow(p.g[h], 1);
+    const Decay lam = decay_of(p.g[h], 1);
     if (tid < p.dk) {
         ks[tid] = load1<E>(p.k, b * p.sk[0] + h * p.sk[1] + tid);
         qs[tid] = load1<E>(p.q, b * p.sq[0] + h * p.sq[1] + tid) * p.scale;
@@ -783,7 +831,7 @@ __global__ __launch_bounds__(256) void k_lin_step(const LinStepParams p) {
                 f4 s = *(const f4*)(S + (int64_t)a * p.dv + c);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[e] = s[e] * lam + ks[a] * v[e];
+                    s[e] = lam.of(s[e], ks[a] * v[e]);
                     o[e] += qs[a] * s[e];
                 }
                 *(f4*)(S + (int64_t)a * p.dv + c) = s;
@@ -793,7 +841,7 @@ __global__ __launch_bounds__(256) void k_lin_step(const LinStepParams p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (c + e < p.dv) {
-                        const float s = S[(int64_t)a * p.dv + c + e] * lam + ks[a] * v[e];
+                        const float s = lam.of(S[(int64_t)a * p.dv + c + e], ks[a] * v[e]);
                         S[(int64_t)a * p.dv + c + e] = s;
                         o[e] += qs[a] * s;
                     }

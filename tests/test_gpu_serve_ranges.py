@@ -119,3 +119,100 @@ def test_small_rows_and_large_weights():
     assert y[0, 0] == 0 and y[0, 1] == float("inf")
     want, tol = ref.product(a, w, sa, sw)
     assert ((y[1].double() - want[1]).abs() <= tol[1]).all()
+
+
+# ---------------------------------------------------------------------------
+# long memories
+# ---------------------------------------------------------------------------
+# A decay close to one is applied thousands of times, so what its rounding adds
+# must not point the same way each time.
+#
+# With new terms of random size each token, n roundings of a state are a random
+# walk of n steps of at most U / sqrt(3) (root mean square): four of its
+# deviations bound the norm over a head's state.
+def walk(n):
+    return 4 * (n / 3) ** 0.5 * ref.U
+
+
+# A state that only decays loses nearly the same number of last places each
+# time, and their fraction is rounded the same way each time: an element may be
+# n U off after n decays.  Over many elements that is next to nothing, so the
+# projection on the state as it should be, sum(x w) / sum(w^2), tells a wrong
+# decay from roundings:
+#  - errors uniform within n U |w| and independent deviate by n U / sqrt(3)
+#    sqrt(sum(w^4)) / sum(w^2), which is n U / sqrt(N) for normally distributed w
+#    (sum(w^4) = 3 N, sum(w^2) = N); four of these;
+#  - a decay by exp(l), |l| small, takes P = |l| / 2 U places of w = 1 and 2 P of
+#    w = 2.  Rounding them has a mean over that range: 1/8 of a place over P at
+#    most from the period that the range cuts, 1/12 over P from the falling
+#    density of w within the periods; together below 0.42 U / P < U (U / |l|),
+#    and never more than U;
+#  - the decay itself is rounded by 2^-23 of its logarithm.
+# decays: [(how many, logarithm of each)].
+def check_decayed(state, S0, decays):
+    total = sum(n * x for n, x in decays)
+    x, want = state.detach().cpu().double(), S0.cpu().double() * float(torch.tensor(total, dtype=torch.float64).exp())
+    if total < -80:      # below fp32's smallest normal number nothing is promised
+        assert float(x.abs().max()) <= 1e-34
+        return
+    n = sum(n for n, _ in decays)
+    own = (2 * abs(total) + 1) * ref.U
+    assert ref.norm_error(x, want) <= n * ref.U + own
+    along = float((x * want).sum() / (want * want).sum()) - 1
+    mean = sum(n * ref.U * min(1, ref.U / abs(x) if x else 0) for n, x in decays)
+    assert abs(along) <= 4 * n * ref.U / want.numel() ** 0.5 + mean + own, (along, mean)
+
+
+LONG = [0.0, -1e-6, -7.3e-6, -1e-5, -(2.0 ** -12), -0.01, -0.68, -0.7, -5.0, float("-inf")]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_thousands_of_tokens_keep_a_long_memory(dtype):
+    H, d, n = len(LONG), 64, 4096
+    g = gen(31)
+    ld = torch.tensor(LONG, device="cuda")
+    q, k, v = (normal(g, 1, H, n, d, dtype=dtype) for _ in range(3))
+    S0 = normal(g, 1, H, d, d, scale=30)
+    state = S0.clone()
+    for i in range(n):
+        out = qx.lin_attn_step(q[:, :, i], k[:, :, i], v[:, :, i], ld, state, scale=0.1)
+    o, S = ref.lin_attn(q, k, v, ld, 0.1, S0)
+    o2, end = qx.lin_attn(q, k, v, ld, scale=0.1, state=S0)
+    for h in range(H):
+        # the state's decay and its new term, two roundings a token
+        assert ref.norm_error(state[:, h], S[:, h]) <= walk(2 * n), h
+        assert ref.norm_error(end[:, h], S[:, h]) <= walk(2 * n), h
+        assert ref.norm_error(out[:, h], o[:, h, -1]) <= walk(2 * n) + 4 * ref.U + (ref.half_ulp(dtype) if dtype != F32 else 0), h
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_state_that_only_decays_token_by_token(dtype):
+    H, n = len(LONG), 8192
+    ld = torch.tensor(LONG, device="cuda")
+    S0 = normal(gen(32), 1, H, 64, 96)
+    state, zero = S0.clone(), torch.zeros(1, H, 96, dtype=dtype, device="cuda")
+    for i in range(n):
+        qx.lin_attn_step(zero[..., :64], zero[..., :64], zero, ld, state)
+    for h, x in enumerate(ld.tolist()):
+        check_decayed(state[:, h], S0[:, h], [(n, x)])
+
+
+# whole sequences, segments and their scan, segments that add up those before them
+@pytest.mark.parametrize("B,H,L,d", [(64, 8, 32768, 64), (1, 8, 1 << 20, 64), (1, 8, 1200, 64), (1, 8, 1 << 18, 128)])
+def test_a_state_that_only_decays_over_a_prompt(B, H, L, d):
+    # one row of zeros is every row of q, k and v
+    x = torch.zeros(d, dtype=BF16, device="cuda").expand(B, H, L, d)
+    logs = [-float(a) / L for a in (0, 1e-3, 3.3e-3, 1e-2, 3.7e-2, 0.13, 0.5, 3.0)]
+    ld = torch.tensor(logs, device="cuda")
+    S0 = normal(gen(33), B, H, d, d)
+    _, end = qx.lin_attn(x, x, x, ld, state=S0)
+    back = qx.lin_attn_backward(x, x, x, x, ld, d_state=S0)[3] if L <= 1 << 18 else None
+    segments = max(qx.plan_lin_attn("bf16", B, H, L, d, d)["k_splits"], 1)
+    of_segment = -(-(L // 32) // segments)          # chunks
+    for h in range(H):
+        x = float(ld[h].double())
+        # the segments before the last one, and its chunks
+        decays = [(segments - 1, 32 * of_segment * x), (L / 32 - (segments - 1) * of_segment, 32 * x)]
+        check_decayed(end[:, h], S0[:, h], decays)
+        if back is not None:
+            check_decayed(back[:, h], S0[:, h], decays)
