@@ -285,8 +285,9 @@ qx_status linear_i8(qx_float_type dt, const void* x, const int8_t* W, const floa
  * for dense arrays, else the (batch, head, row) strides of Q, K, V, O in
  * elements, 12 values, each in [0, 2^40]; the last dimension is contiguous;
  * inputs may have strides of 0, elements of O may not share addresses.
- * dk, dv in [1, 256], L in [0, 2^30], B H <= 2^24 (below 2^21 for one token with
- * dv 256), any finite scale.
+ * dk, dv in [1, 256], L in [0, 2^30], any finite scale, B H <= 2^24; where dv > 64
+ * or a head size is no multiple of 8, B H ceil(dv / 128) < 2^24 (gradients: dk
+ * counts like dv); for one token B H ceil(dv / 32) < 2^24.
  * FP32 operands of magnitude 2^127 and more count as infinite, and of those
  * below 2^-109 bits under 2^-133 are lost. */
 qx_status lin_attn(qx_float_type dt, const void* Q, const void* K, const void* V, const float* log_decay,
@@ -302,7 +303,11 @@ qx_status lin_attn_step(qx_float_type dt, const void* q, const void* k, const vo
                         float scale, void* stream);
 
 /* Gradients of lin_attn: from dO, and dS_out (NULL: zeros), those of Q, K, V
- * and S0 (dS0 may be NULL; it may be the array dS_out).  Rows behind a
+ * and S0 (dS0 may be NULL; it may be the array dS_out): with
+ *   G_{n-1} = scale q_{n-1}^T dO_{n-1} + dS_out,
+ *   G_i = scale q_i^T dO_i + exp(log_decay[h]) G_{i+1},
+ * dQ_i = scale dO_i S_i^T, dK_i = V_i G_i^T, dV_i = K_i G_i, dS0 = exp(log_decay[h])
+ * G_0 (dS_out for an empty sequence).  Rows behind a
  * sequence's end are neither read nor written.  log_decay is a constant.
  * strides: NULL or those of Q, K, V, dO, dQ, dK, dV, 21 values.  A gradient
  * is that of its own element: inputs read through strides of 0 get no sums. */

@@ -74,7 +74,7 @@ qx_status check_ws(const Plan& pl, const void* ws, int64_t bytes) {
 
 // A grid holds fewer than 2^32 threads.
 qx_status check_grid(int64_t workgroups, int64_t threads) {
-    if (workgroups > 0xFFFFFFFFll / threads) return plan_fail(QX_ERR_UNSUPPORTED, "B*H*L is too large for one launch");
+    if (workgroups > 0xFFFFFFFFll / threads) return plan_fail(QX_ERR_UNSUPPORTED, "B*H is too large for one launch over heads of these sizes");
     return QX_OK;
 }
 
@@ -391,7 +391,8 @@ qx_status plan_lin_attn(Plan* pl, const LinSpec& s, const int64_t* strides, bool
 }
 
 // inputs {Q, K, V, dO, log_decay, S0, dS, lens, dQ, dK, dS0}, output dV.
-// With G_i = scale q_i^T dO_i + lambda G_{i+1}, G_n = dS behind the end:
+// With G_{n-1} = scale q_{n-1}^T dO_{n-1} + dS, G_i = scale q_i^T dO_i + lambda G_{i+1},
+// dS0 = lambda G_0 (dS where there is no token):
 //   dQ_i = scale dO_i S_i^T        the forward recurrence on (dO, V, K), S0^T
 //   dK_i = V_i G_i^T, dV_i = K_i G_i   backwards on (V, dO, Q), dS^T and (K, Q, dO), dS
 qx_status plan_lin_backward(Plan* pl, const LinSpec& s, const int64_t* strides, bool state, bool d_end, bool lens,

@@ -1,0 +1,32 @@
+"""Linear attention on the host: the largest numbers of heads that are
+documented, on both sides, and calls with a missing operand."""
+import pytest
+
+import test_serve_host as host
+from paper_2606_09905_amd import qx
+from test_serve_host import double  # noqa: F401  (a fixture)
+
+# (dk, dv): heads that a prompt takes, that its gradients take
+HEADS = [((64, 64), 1 << 24, 1 << 24), ((8, 56), 1 << 24, 1 << 24),
+         ((64, 72), (1 << 24) - 1, (1 << 24) - 1), ((72, 64), 1 << 24, (1 << 24) - 1), ((128, 128), (1 << 24) - 1, (1 << 24) - 1),
+         ((33, 64), (1 << 24) - 1, (1 << 24) - 1), ((64, 136), (1 << 23) - 1, (1 << 23) - 1),
+         ((256, 64), 1 << 24, (1 << 23) - 1), ((256, 256), (1 << 23) - 1, (1 << 23) - 1)]
+
+
+def _both_sides(call, heads, **kw):
+    assert call(B=1, H=heads, **kw) == qx.OK, host.last()
+    assert call(B=1, H=heads + 1, **kw) == qx.ERR_UNSUPPORTED
+    # whatever bounds it, the message names the heads, and nothing that the call does not have
+    assert "H" in host.last() and "L" not in host.last(), host.last()
+
+
+@pytest.mark.parametrize("d,prompt,gradients", HEADS)
+@pytest.mark.parametrize("dt", [0, 2])
+def test_heads_of_prompts_and_gradients(double, dt, d, prompt, gradients):  # noqa: F811
+    _both_sides(lambda **kw: host.attn(double, **kw), prompt, dt=dt, n=32, dk=d[0], dv=d[1])
+    _both_sides(lambda **kw: host.back(double, **kw), gradients, dt=dt, n=32, dk=d[0], dv=d[1])
+
+
+@pytest.mark.parametrize("dv", [1, 32, 33, 128, 250, 256])
+def test_heads_of_one_token(double, dv):  # noqa: F811
+    _both_sides(lambda **kw: host.step(double, **kw), ((1 << 24) - 1) // -(-dv // 32), dk=64, dv=dv)
