@@ -30,3 +30,18 @@ def test_heads_of_prompts_and_gradients(double, dt, d, prompt, gradients):  # no
 @pytest.mark.parametrize("dv", [1, 32, 33, 128, 250, 256])
 def test_heads_of_one_token(double, dv):  # noqa: F811
     _both_sides(lambda **kw: host.step(double, **kw), ((1 << 24) - 1) // -(-dv // 32), dk=64, dv=dv)
+
+
+@pytest.mark.parametrize("name,args", [("quant", "x q s"), ("product", "a w sa sw y"), ("linear", "x w sw y ws"),
+                                       ("attn", "q k v g o"), ("step", "q k v g s o"),
+                                       ("back", "q k v do g dq dk_ dv_ ws")])
+@pytest.mark.parametrize("n", [40, 600])
+def test_nothing_is_enqueued_without_an_operand(double, name, args, n):  # noqa: F811
+    kw = dict(n=n) if name in ("attn", "back") else {}
+    need = name != "back" or qx.plan_lin_attn_backward("bf16", 2, 3, n, 64, 64)["workspace_bytes"]
+    for arg in args.split():
+        if arg == "ws" and not need:
+            continue
+        before = qx.testing_counters()["launches"]
+        assert host.CALLS[name](double, **{arg: None}, **kw) == qx.ERR_INVALID_ARG, arg
+        assert host.last() and qx.testing_counters()["launches"] == before, arg
