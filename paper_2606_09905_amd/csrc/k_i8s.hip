@@ -556,10 +556,11 @@ void build_quant_i8(const QuantI8Params& p0, LaunchRec* rec) {
     rec->set_params(p);
 }
 
-// Few rows go to the kernel that is made for them (these / 64 x 64 tiles, us:
-// 64 x 8192 x 4096 25.3 / 15.7, 48 x 8192 x 4096 21.5 / 15.5, 24 x 4096 x 4096
-// 9.1 / 14.6, 24 x 1024 x 1024 7.4 / 6.4).
-bool rows_i8s(int64_t M, int64_t N) { return M <= 16 || (M <= 32 && N >= 2048); }
+// Few rows go to the kernel that is made for them, whose waves share K (these /
+// 64 x 64 tiles, us: 17 x 256 x 256 3.6 / 3.8, 24 x 1024 x 1024 4.3 / 5.9, 24 x
+// 1024 x 8192 12.2 / 22.7, 32 x 64 x 16384 23.5 / 41.2, 32 x 4096 x 4096 8.8 /
+// 14.0; 48 x 8192 x 4096 21.5 / 15.5, 64 x 8192 x 4096 25.3 / 15.7).
+bool rows_i8s(int64_t M) { return M <= 32; }
 
 // Whether the product quantises its activations itself (x, no A).  Its threads
 // are shared among the next power of two of rows, each of whose threads hold
@@ -573,7 +574,7 @@ bool fused_i8s(int64_t M, int64_t K) {
 void build_gemm_i8s(const GemmI8sParams& p0, bool aligned, LaunchRec* rec, int* tile_m, int* tile_n, int* tile_k) {
     GemmI8sParams p = p0;
     *tile_k = 128;
-    if (rows_i8s(p.M, p.N)) {
+    if (rows_i8s(p.M)) {
         const bool fused = p.lda == 0;   // no A: x
         // 32 rows of W a workgroup, which halves the reads of A, once there
         // is one for every CU (4096 k, 16 / 32 rows, us: 24 x 8192 16.0 / 12.9,

@@ -505,7 +505,7 @@ void build_conv_prep_limb(const ConvLimbPrepParams& p, LaunchRec* rec);
 bool build_gemm_i8nt(int32_t route, const GemmParams& p, int batch, LaunchRec* rec);
 // 8-bit rows and their scaled product (k_i8s.hip).
 void build_quant_i8(const QuantI8Params& p, LaunchRec* rec);
-bool rows_i8s(int64_t M, int64_t N);
+bool rows_i8s(int64_t M);
 bool fused_i8s(int64_t M, int64_t K);
 void build_gemm_i8s(const GemmI8sParams& p, bool aligned, LaunchRec* rec, int* tile_m, int* tile_n, int* tile_k);
 // Linear attention with decay (k_lin.hip): the launch shape, the launches

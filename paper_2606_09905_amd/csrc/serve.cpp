@@ -197,7 +197,7 @@ qx_status plan_linear_i8(Plan* pl, int32_t type, int64_t M, int64_t N, int64_t K
     // Rows of W that start anywhere cannot go to LDS directly: beyond a few
     // tokens they are copied to whole rows beside the quantisation (777 x 1000
     // x 1501: 16.4 -> 14.8 us)
-    const bool copy = K % 16 != 0 && !rows_i8s(M, N);
+    const bool copy = K % 16 != 0 && !rows_i8s(M);
     uint64_t w_off = 0;
     if (copy) {
         w_off = round_up(ws, 256);

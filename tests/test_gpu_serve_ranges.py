@@ -121,6 +121,25 @@ def test_small_rows_and_large_weights():
     assert ((y[1].double() - want[1]).abs() <= tol[1]).all()
 
 
+# on each side of the rules by which a kernel is chosen
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(17, 1, 64), (24, 100, 8192), (32, 1000, 300), (32, 2047, 1501), (33, 2047, 1501),
+                                   (64, 16383, 129), (64, 16400, 129), (512, 16400, 65), (513, 16400, 65)])
+def test_layers_on_each_side_of_a_rule(dtype, M, N, K):
+    g = gen(M + N)
+    x = normal(g, M, K, dtype=dtype)
+    w = torch.randint(-128, 128, (N, K), generator=g, dtype=torch.int32).to(torch.int8).cuda()
+    sw = torch.rand(N, generator=g).cuda() * 1e-2
+    y = qx.linear_i8(x, w, sw)
+    a, sa = qx.quantize_rows_i8(x)
+    assert torch.equal(y, qx.qgemm_i8_scaled(a, w, sa, sw, dtype=dtype))
+    rows = [0, M // 2, M - 1]
+    want, tol = ref.product(a[rows], w, sa[rows], sw)
+    floor = 2.0 ** -25 if dtype == F16 else 0
+    tol = tol + (ref.half_ulp(dtype) * (want.abs() + tol) if dtype != F32 else 0) + floor
+    assert ((y[rows].cpu().double() - want).abs() <= tol).all()
+
+
 # ---------------------------------------------------------------------------
 # long memories
 # ---------------------------------------------------------------------------

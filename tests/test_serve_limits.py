@@ -1,5 +1,6 @@
-"""Linear attention on the host: the largest numbers of heads that are
-documented, on both sides, and calls with a missing operand."""
+"""On the host: the largest numbers of heads that linear attention is
+documented to take, on both sides; calls with a missing operand; and which of
+the 8-bit kernels a size gets."""
 import pytest
 
 import test_serve_host as host
@@ -45,3 +46,11 @@ def test_nothing_is_enqueued_without_an_operand(double, name, args, n):  # noqa:
         before = qx.testing_counters()["launches"]
         assert host.CALLS[name](double, **{arg: None}, **kw) == qx.ERR_INVALID_ARG, arg
         assert host.last() and qx.testing_counters()["launches"] == before, arg
+
+
+@pytest.mark.parametrize("N", [1, 64, 1024, 2047, 2048, 9000])
+@pytest.mark.parametrize("K", [64, 1501, 8192, 131071])
+def test_few_rows_go_to_the_kernel_whose_waves_share_k(N, K):
+    for f in (qx.plan_gemm_i8_scaled, qx.plan_linear_i8):
+        assert [f("bf16", M, N, K)["tile_m"] for M in (16, 17, 24, 32)] == [16, 32, 32, 32]
+        assert f("bf16", 33, N, K)["tile_m"] >= 64
