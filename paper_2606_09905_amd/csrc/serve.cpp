@@ -195,9 +195,13 @@ qx_status plan_linear_i8(Plan* pl, int32_t type, int64_t M, int64_t N, int64_t K
     q.rows = M; q.cols = K; q.ld = ldx; q.ldq = ldq;
     q.type = type;
     // Rows of W that start anywhere cannot go to LDS directly: beyond a few
-    // tokens they are copied to whole rows beside the quantisation (777 x 1000
-    // x 1501: 16.4 -> 14.8 us)
-    const bool copy = K % 16 != 0 && !rows_i8s(M);
+    // tokens they are copied to whole rows beside the quantisation, but not many
+    // rows for few tokens, whose copies take longer than the products gain
+    // (copied / not, us: 777 x 1000 x 1501 14.8 / 16.4, 33 x 1000 x 4099 19.9 /
+    // 24.8, 256 x 12288 x 8001 86.8 / 94.3, 33 x 16384 x 1001 17.3 / 13.3, 256 x
+    // 32768 x 4099 102 / 82, 33 x 32768 x 8001 166 / 79, 512 x 16384 x 4099 77.0
+    // / 76.2, 1024 x 16384 x 4099 113 / 117, 2048 x 32768 x 1001 166 / 198)
+    const bool copy = K % 16 != 0 && !rows_i8s(M) && (M > 512 || N < 16384);
     uint64_t w_off = 0;
     if (copy) {
         w_off = round_up(ws, 256);

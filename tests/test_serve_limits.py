@@ -54,3 +54,11 @@ def test_few_rows_go_to_the_kernel_whose_waves_share_k(N, K):
     for f in (qx.plan_gemm_i8_scaled, qx.plan_linear_i8):
         assert [f("bf16", M, N, K)["tile_m"] for M in (16, 17, 24, 32)] == [16, 32, 32, 32]
         assert f("bf16", 33, N, K)["tile_m"] >= 64
+
+
+@pytest.mark.parametrize("M,N,K,copied", [(777, 1000, 1501, True), (33, 16383, 1001, True), (33, 16384, 1001, False),
+                                          (512, 40000, 4099, False), (513, 40000, 4099, True), (33, 1000, 1008, False),
+                                          (32, 1000, 1501, False)])
+def test_weights_are_copied_where_it_pays(M, N, K, copied):
+    need = qx.plan_linear_i8("bf16", M, N, K)["workspace_bytes"]
+    assert (need >= N * K) == copied and need >= M * K
