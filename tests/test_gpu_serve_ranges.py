@@ -235,3 +235,30 @@ def test_a_state_that_only_decays_over_a_prompt(B, H, L, d):
         check_decayed(end[:, h], S0[:, h], decays)
         if back is not None:
             check_decayed(back[:, h], S0[:, h], decays)
+
+
+def test_ragged_calls_that_make_their_results_in_a_graph():
+    B, H, L, d = 3, 2, 600, 64
+    g = gen(41)
+    q, k, v, do = (normal(g, B, H, L, d, dtype=BF16) for _ in range(4))
+    ld = torch.tensor([-0.1, -0.01], device="cuda")
+    lens = torch.tensor([L, 5, 0], dtype=torch.int32, device="cuda")
+
+    def work():
+        out, end = qx.lin_attn(q, k, v, ld, lens=lens)
+        return (out, end, *qx.lin_attn_backward(q, k, v, do, ld, lens=lens))
+
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = work()
+    for rep in range(4):
+        lens.copy_(torch.tensor([[L, 5, 0], [1, L, 300], [0, 0, L], [L - 1, 33, 2]][rep], dtype=torch.int32))
+        q.copy_(normal(gen(rep), B, H, L, d, dtype=BF16))
+        for t in res:
+            t.fill_(3)
+        graph.replay()
+        for a, b in zip(res, work()):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
