@@ -202,8 +202,8 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // BM x BN tiles, WM x WN waves, K in tiles of 128 bytes through a ring of
-// STAGES.  Bound by the matrix cores and their power at 256 x 256 (8192^3 535
-// us, 2050 TOPS; without its loads 386, without its LDS reads 522, the products
+// STAGES.  Bound by the matrix cores and their power at 256 x 256 (8192^3 541
+// us, 2030 TOPS; without its loads 386, without its LDS reads 522, the products
 // alone 421): spreading the loads over the products, by halves of the waves
 // too, fragments read a step ahead through a ring of four 64-byte tiles, and
 // four waves of 128 x 128 all measured 525 to 650.  ALIGNED: rows start at

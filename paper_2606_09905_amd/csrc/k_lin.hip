@@ -40,7 +40,8 @@
 // Z a second time (64 heads x 8192 x 128: states 66 us for 268 MB, chunks 160
 // us for 537 MB, 3.4 TB/s; three streams read and one written in the same
 // tiles without any work take 140 us); fp32 the matrix cores and the splitting
-// of values into terms, six products for one (64 heads x 1999 x 96 x 80: 117 us).
+// of values into terms, six products for one (64 heads x 1999 x 96 x 80: 115 us),
+// and registers in scratch (42 a lane there; 14 at dx 64 with two waves).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -140,7 +141,7 @@ __device__ __forceinline__ Decay decay_of(float g, int n) {
 // The factors exp(g n) for one step of n tokens after the other: of the two
 // floats around it now one, now the other, so that the product of any number
 // of them is a rounding off.  (The two terms above for each element of the
-// state cost 5% to 37% of the time of all chunks; a wave's these are two scalar adds.)
+// state cost up to 37% of the time of all chunks; of these a wave has two scalar adds.)
 struct Factors {
     uint32_t lo, part, at;   // the smaller float; how far, in 2^-32, exp(g n) lies past it; what has gathered
     __device__ __forceinline__ float next() {

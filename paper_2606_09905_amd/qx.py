@@ -370,7 +370,8 @@ def pool2x2(x, out=None, stream=None):
 #
 # A token's step is a few microseconds on the GPU, so these keep the host's
 # part short: one condition over all operands, and the checks one by one only
-# where it fails, to say what is wrong.
+# where it fails, to say what is wrong.  None of them records an autograd
+# graph, whatever its operands require.
 # ---------------------------------------------------------------------------
 _ftype = {}    # torch dtype -> qx_float_type
 _need = {}     # (query, type, sizes) -> workspace bytes
@@ -555,7 +556,8 @@ def lin_attn(q, k, v, log_decay, scale: float = 1.0, state=None, lens=None, out=
     a contiguous last dimension; log_decay [H], state [B, H, dk, dv] float32
     (None: zeros); lens [B] int32 (None: L), rows of `out` behind a sequence's
     end are left as they were, zeros where the call makes it.  Returns (out,
-    state after the last token); out_state may be `state` itself."""
+    state after the last token); out_state may be `state` itself.  Records no
+    autograd graph: lin_attn_backward gives the gradients."""
     T = q.dtype
     dt = _float_type(T, "q")
     shape = q.shape
