@@ -125,17 +125,16 @@ __device__ __forceinline__ float decay_pow(float g, int n) {
 // One token's: s exp(g) + more, as s + (s (exp(g) - 1) + more) where exp(g) is
 // more than a half.
 struct Decay {
-    float f;      // exp(g n) - 1, or exp(g n)
+    float f;      // exp(g) - 1, or exp(g)
     bool near;    // (the same for all threads of a head)
     __device__ __forceinline__ float of(float s, float more) const {
         const float t = __builtin_fmaf(s, f, more);
         return near ? s + t : t;
     }
 };
-__device__ __forceinline__ Decay decay_of(float g, int n) {
-    const double x = (double)g * n;
-    const bool near = x > -0.69;
-    const float less = expm1f((float)x), whole = decay_pow(g, n);   // (both: a branch would hold back the loads behind it)
+__device__ __forceinline__ Decay decay_of(float g) {
+    const bool near = g > -0.69f;
+    const float less = expm1f(g), whole = decay_pow(g, 1);   // (both: a branch would hold back the loads behind it)
     return {near ? less : whole, near};
 }
 // The factors exp(g n) for one step of n tokens after the other: of the two
@@ -760,7 +759,7 @@ __global__ __launch_bounds__(256) void k_lin_scan(const LinParams p) {
     const int c = (zt * waves + wave) * 32 + (lane & 31), a0 = 32 * (grp >> 2) + 8 * (grp & 3) + 4 * (lane >> 5);
     if (c >= p.dz) return;
     const int len = p.lens ? min(max(p.lens[b], 0), p.L) : p.L;
-    const Decay lam = decay_of(p.g[h], p.seg_len);
+    Factors of_segments = factors_of(p.g[h], p.seg_len);   // (those of the chunks' launch: the same bits as without a scan)
     const int ra = p.s_t ? 1 : p.dz, rc = p.s_t ? p.dx : 1;
     f4 cur;
 #pragma unroll
@@ -782,8 +781,9 @@ __global__ __launch_bounds__(256) void k_lin_scan(const LinParams p) {
         for (int k = 0; k < AT_ONCE; ++k)
             if (s0 + k < n) {
                 *(f4*)(u + (s0 + k) * per * 4) = cur;
+                const float lam = of_segments.next();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) cur[e] = lam.of(cur[e], v[k][e]);
+                for (int e = 0; e < 4; ++e) cur[e] = cur[e] * lam + v[k][e];
             }
     }
 }
@@ -816,7 +816,7 @@ __global__ __launch_bounds__(256) void k_lin_step(const LinStepParams p) {
     float* S = p.S + bh * p.dk * p.dv;
     // full vectors where rows keep their 16 bytes, else element by element
     const bool vec = p.dv % 4 == 0 && ((uintptr_t)p.S & 15) == 0;
-    const Decay lam = decay_of(p.g[h], 1);
+    const Decay lam = decay_of(p.g[h]);
     if (tid < p.dk) {
         ks[tid] = load1<E>(p.k, b * p.sk[0] + h * p.sk[1] + tid);
         qs[tid] = load1<E>(p.q, b * p.sq[0] + h * p.sq[1] + tid) * p.scale;

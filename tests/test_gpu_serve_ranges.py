@@ -262,3 +262,18 @@ def test_ragged_calls_that_make_their_results_in_a_graph():
         for a, b in zip(res, work()):
             assert torch.equal(a, b)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("L,d", [(1000, 64), (1200, 64), (2000, 128)])
+def test_a_state_in_place_has_the_bits_of_one_apart(dtype, L, d):
+    # few segments add up the states before them, but not where the state is in place
+    H = len(LONG)
+    g = gen(L)
+    q, k, v = (normal(g, 1, H, L, d, dtype=dtype) for _ in range(3))
+    ld = torch.tensor(LONG, device="cuda")
+    S0 = normal(g, 1, H, d, d, scale=10)
+    out, end = qx.lin_attn(q, k, v, ld, state=S0)
+    state = S0.clone()
+    got, _ = qx.lin_attn(q, k, v, ld, state=state, out_state=state)
+    assert torch.equal(got, out) and torch.equal(state, end)
